@@ -27,13 +27,14 @@ struct Running {
 __device__ __forceinline__ float term(float z, float m, float c) { return __builtin_amdgcn_exp2f((z - m) * c); }
 
 // The same for many z and one m: exp2 of a fused z c - m c, which misses the
-// factor by the rounding of m c alone; `missed` makes up for it.  Where m c
-// overflows, so could z c with the other sign: not for such m.
+// factor by the rounding of m c alone; `missed` makes up for it.  That rounding
+// is in the exponent, up to |m c| 2^-24: only while it stays below 1 are both
+// factors near 1, past 126 one would be 0 and the other infinite.
 struct Terms {
   float c, m, mc, missed;
   bool fused;
   __device__ __forceinline__ Terms(float m_, float c_) : c(c_), m(m_), mc(m_ * c_) {
-    fused = fabsf(mc) < 1e30f;
+    fused = fabsf(mc) < 16777216.f;
     missed = fused ? __builtin_amdgcn_exp2f(-fmaf(m, c, -mc)) : 1.f;
   }
   __device__ __forceinline__ float near(float z) const { return __builtin_amdgcn_exp2f(fmaf(z, c, -mc)); }

@@ -1,0 +1,87 @@
+"""The training operators (include/spardl_train.h) at the ends of their
+arguments' ranges, on the GPU, against their definitions in 64 bits.  Every
+tolerance is a bound from tests/train_ref.py or derived where it stands."""
+
+import math
+import zlib
+
+import pytest
+import torch
+
+from paper_2304_00737_amd import train
+from tests import train_ref as ref
+from tests.gpu_util import log
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def _gen(*key):
+    return torch.Generator(device=DEV).manual_seed(zlib.crc32(repr(key).encode()))
+
+
+def _randn(g, *shape):
+    return torch.randn(*shape, generator=g, device=DEV)
+
+
+# ------------------------------------------------------------------ distillation
+
+def _check_distill(z, idx, val, dloss, t):
+    """All calls on the same rows against the 64-bit form."""
+    rows, vocab = z.shape
+    ws = train.distill_workspace(rows, vocab)
+    wl, wst, wd, bl, bst, bd = ref.distill(z, idx, val, t, dloss)
+    loss, stats, d = torch.empty(rows, device=DEV), torch.empty(rows, 2, device=DEV), torch.empty_like(z)
+    train.distill_loss(z, idx, val, loss, stats, ws, temperature=t)
+    ref.assert_within("loss", loss, wl, bl, torch.float32)
+    ref.assert_within("stats", stats, wst, bst, torch.float32)
+    train.distill_backward(z, idx, val, stats, dloss, d, temperature=t)
+    ref.assert_within("dlogits", d, wd, bd, z.dtype)
+    over = z.clone()
+    train.distill_backward(over, idx, val, stats, dloss, over, temperature=t)
+    assert torch.equal(over, d)
+    for t_ in (loss, stats, d):
+        t_.fill_(float("nan"))
+    train.distill_loss_backward(z, idx, val, dloss, loss, stats, d, ws, temperature=t)
+    ref.assert_within("fused loss", loss, wl, bl, torch.float32)
+    ref.assert_within("fused stats", stats, wst, bst, torch.float32)
+    ref.assert_within("fused dlogits", d, wd, bd, z.dtype)
+
+
+# rows x vocabulary: one chunk of logits a thread; several, in every form of rows held in registers; segments; and
+# (in 32 bits) rows read twice by one workgroup
+MASKED = [(*size, dtype) for size in ((9, 1000), (70, 8193), (66, 20001), (70, 50257), (130, 131072), (5, 131073))
+          for dtype in (torch.bfloat16, torch.float32)] + [(2050, 66000, torch.float32)]
+
+
+@pytest.mark.parametrize("rows,vocab,dtype", MASKED)
+def test_distill_large_masks(rows, vocab, dtype):
+    """Finite masks of any size, on whole rows, on runs that fill some threads' share, and far below one large logit."""
+    top = 20
+    for mask in (-1e9, -1e10, -1e20, -1e30):
+        for t in ((1.0,) if rows > 2000 else (0.5, 1.0, 2.0)):
+            log(f"distill masked {rows} x {vocab} {dtype} mask {mask} t {t}")
+            g = _gen("masks", rows, vocab, mask, t)
+            z = (3 * _randn(g, rows, vocab)).to(dtype)
+            idx = torch.randint(vocab, (rows, top), generator=g, device=DEV).to(torch.int32)
+            val = 4 * _randn(g, rows, top)
+            z[0::4, vocab - vocab // 8:] = mask           # columns that pad the vocabulary
+            z[1::4] = mask                                # a mask that leaves nothing: q is uniform
+            z[2::4, ::3] = mask
+            z[3::4, vocab // 2] = -mask                   # all the others have no probability
+            _check_distill(z, idx, val, 1 + torch.rand(rows, generator=g, device=DEV), t)
+
+
+@pytest.mark.parametrize("rows,vocab", [(9, 1000), (70, 50257), (5, 131073)])
+def test_distill_large_logits_over_a_small_temperature(rows, vocab):
+    """fp16 masks of its lowest order at temperatures that take them past every bound of a fused exponent."""
+    top = 20
+    for t in (2.0 ** -10, 2.0 ** -16, 2.0 ** -30):
+        g = _gen("cold", rows, vocab, t)
+        z = (3 * t * _randn(g, rows, vocab)).to(torch.float16)
+        idx = torch.randint(vocab, (rows, top), generator=g, device=DEV).to(torch.int32)
+        val = 4 * t * _randn(g, rows, top)
+        z[0::3, : vocab // 2] = -60000.0
+        z[1::3] = -60000.0
+        _check_distill(z, idx, val, (1 + torch.rand(rows, generator=g, device=DEV)) / t, t)
