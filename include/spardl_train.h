@@ -90,8 +90,8 @@ int spardl_rms_norm_backward(const void* dy, int64_t ld_dy, const void* sum, int
  * dlogits may be logits itself (with its ld): the logits are then replaced.
  * Errors: EINVAL for NULL pointers, rows < 0, vocab < 1, top outside
  * [1, SPARDL_DISTILL_MAX_TOP], ld below the row's length, a temperature that
- * is not positive and finite, an unknown dtype, or a NULL or misaligned ws;
- * ECAPACITY. */
+ * is not a positive normal number (2^-126 at least, finite), an unknown dtype,
+ * or a NULL or misaligned ws; ECAPACITY. */
 size_t spardl_distill_workspace_bytes(int64_t rows, int32_t vocab);
 int spardl_distill_loss(const void* logits, int64_t ld, const int32_t* top_idx, const float* top_val, int64_t ld_top,
                         int64_t rows, int32_t vocab, int32_t top, float temperature, float* loss, float* stats,

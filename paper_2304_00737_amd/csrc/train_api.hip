@@ -76,7 +76,7 @@ namespace {
 int distill_check(const Distill& d) {
   if (d.rows < 0 || d.rows > kMaxRows || d.vocab < 1 || d.top < 1 || d.top > SPARDL_DISTILL_MAX_TOP || !known(d.dtype))
     return SPARDL_EINVAL;
-  if (!(d.temperature > 0.f) || std::isinf(d.temperature)) return SPARDL_EINVAL;
+  if (!std::isnormal(d.temperature) || d.temperature < 0.f) return SPARDL_EINVAL;     // log2(e) / it is finite
   if (!matrix(d.logits, d.ld, d.rows, d.vocab, size_of(d.dtype)) || !matrix(d.top_idx, d.ld_top, d.rows, d.top, 4) ||
       !matrix(d.top_val, d.ld_top, d.rows, d.top, 4))
     return SPARDL_EINVAL;

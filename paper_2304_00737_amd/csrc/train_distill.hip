@@ -105,6 +105,8 @@ __device__ void fetch_list(List& L, const T* row, const int32_t* idx, const floa
 
 // The list's probabilities, and whether the row has any slot; loss: the row's
 // loss, valid in every thread.  A thread works on the slots that it fetched.
+// The loss is t times the sum of p (t log p - t log q): 1 / t and t^2, which
+// pass the range of 32 bits long before t does, occur nowhere.
 template <int THREADS>
 __device__ bool settle_list(List& L, int top, float t, Running q, bool want_loss, float* loss) {
   const float c = kLog2e / t;
@@ -127,15 +129,15 @@ __device__ bool settle_list(List& L, int top, float t, Running q, bool want_loss
   total = group_sum<THREADS>(total, L.red);
   any = any || total != total;
   __syncthreads();
-  const float inv = 1.f / total, logt = logf(total), logs = logf(q.s), it = 1.f / t;
+  const float inv = 1.f / total, logs = t * (logf(q.s) - logf(total));
   float sum = 0.f;
   for (int k = threadIdx.x; k < top; k += THREADS) {
     const float u = L.p[k];
     const float p = u == -INFINITY ? 0.f : term(u, m, c) * inv;
     L.p[k] = p;
-    if (want_loss && !(p <= 0.f)) sum += p * (((u - m) * it - logt) - ((L.z[k] - q.m) * it - logs));
+    if (want_loss && !(p <= 0.f)) sum += p * (((u - m) - (L.z[k] - q.m)) + logs);
   }
-  if (want_loss) *loss = any ? t * t * group_sum<THREADS>(sum, L.red) : 0.f;
+  if (want_loss) *loss = any ? t * group_sum<THREADS>(sum, L.red) : 0.f;
   __syncthreads();
   return any;
 }

@@ -85,3 +85,14 @@ def test_distill_large_logits_over_a_small_temperature(rows, vocab):
         z[0::3, : vocab // 2] = -60000.0
         z[1::3] = -60000.0
         _check_distill(z, idx, val, (1 + torch.rand(rows, generator=g, device=DEV)) / t, t)
+
+
+@pytest.mark.parametrize("rows,vocab,top", [(5, 20, 20), (9, 1000, 20), (70, 8193, 7), (70, 50257, 20), (5, 131073, 20)])
+def test_distill_temperatures(rows, vocab, top):
+    """Temperatures whose square or reciprocal 32 bits do not hold: the loss is of order t to t^2."""
+    for t in (2.0 ** -126, 2.0 ** -90, 2.0 ** -80, 2.0 ** -60, 2.0 ** 60, 2.0 ** 70):
+        log(f"distill {rows} x {vocab} t {t}")
+        g = _gen("temperature", rows, vocab, t)
+        z = 3 * _randn(g, rows, vocab)
+        idx = torch.stack([torch.randperm(vocab, generator=g, device=DEV)[:top] for _ in range(rows)]).to(torch.int32)
+        _check_distill(z, idx, 4 * _randn(g, rows, top), 1 + torch.rand(rows, generator=g, device=DEV), t)

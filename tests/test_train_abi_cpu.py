@@ -95,6 +95,16 @@ def test_distill_refusals():
 
 
 @needs_lib
+@pytest.mark.parametrize("t", [2.0 ** -127, 2.0 ** -149, -2.0 ** -127, -0.0, float("-inf")])
+def test_distill_refuses_a_temperature_without_a_finite_reciprocal(t):
+    _, lib = _binding()
+    assert lib.spardl_distill_loss(P, 100, P, P, 4, 3, 100, 4, t, P, P, 0, P, 1 << 20, None) == EINVAL
+    assert lib.spardl_distill_backward(P, 100, P, P, 4, P, P, 3, 100, 4, t, P, 100, 0, None) == EINVAL
+    assert lib.spardl_distill_loss_backward(P, 100, P, P, 4, P, 3, 100, 4, t, P, P, P, 100, 0, P, 1 << 20, None) == EINVAL
+    assert lib.spardl_distill_loss(P, 100, P, P, 4, 0, 100, 4, 2.0 ** -126, P, P, 0, P, 1 << 20, None) == OK
+
+
+@needs_lib
 def test_ffn_refusals():
     _, lib = _binding()
 
