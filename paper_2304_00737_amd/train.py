@@ -2,8 +2,8 @@
 training operators of include/spardl_train.h, whose weight gradients the calls
 of spardl.py synchronise.
 
-Every function takes torch tensors for device buffers, outputs included, and
-raises SpardlError on failure.  Matrices are 2-d with contiguous rows (any row
+Every function takes torch tensors for device buffers, outputs included, all on
+the current device, and raises SpardlError on failure.  Matrices are 2-d with contiguous rows (any row
 stride); types are bfloat16, float16 and, except for the feed-forward block,
 float32.  All compute runs in the HIP kernels of the library; there is no
 fallback: if it is missing, importing this module fails.
@@ -78,6 +78,8 @@ def _mat(fn: str, name: str, t, shape, dtype):
     if t is None:
         return None, shape[1]
     if t.shape == shape and t.dtype is dtype:
+        if t.is_contiguous():
+            return t.data_ptr(), shape[1]
         strides = t.stride()
         if strides[1] == 1 or shape[1] == 1:
             return t.data_ptr(), strides[0] if shape[0] > 1 else shape[1]
@@ -97,13 +99,23 @@ def _ws(ws):
     return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
 
 
-# the current stream's handle by the shortest way: small calls are bound by what precedes their launch
+# the current device and its stream's handle by the shortest way: small calls are bound by what precedes their launch
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _on(stream, t) -> int:
+def _on(fn: str, stream, *tensors) -> int:
+    """The stream's handle, after the check that every tensor (or None) is on the device that the launch goes to."""
+    at = _current_device() if tensors[0].is_cuda else -1
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            at = -1
+            break
+    if at < 0:
+        _refuse(fn, "all tensors must be on the current GPU, are on "
+                    f"{sorted({str(t.device) for t in tensors if t is not None})}")
     if stream is None and _raw_stream is not None:
-        return _raw_stream(t.get_device())
+        return _raw_stream(at)
     return _stream(stream)
 
 
@@ -122,7 +134,7 @@ def rms_norm(x, res, weight, sum, y, rstd=None, *, eps: float = 1e-6, stream=Non
     _check(fn, _lib.spardl_rms_norm(*_mat(fn, "x", x, shape, dt), *_mat(fn, "res", res, shape, dt),
                                     _vec(fn, "weight", weight, dim, dt), *_mat(fn, "sum", sum, shape, dt),
                                     *_mat(fn, "y", y, shape, dt), _vec(fn, "rstd", rstd, rows), rows, dim, eps,
-                                    _type(fn, x), _on(stream, x)))
+                                    _type(fn, x), _on(fn, stream, x, res, weight, sum, y, rstd)))
 
 
 def rms_norm_workspace(rows: int, dim: int, device="cuda"):
@@ -137,7 +149,8 @@ def rms_norm_backward(dy, sum, weight, rstd, dx, dweight, ws, dsum=None, *, stre
     _check(fn, _lib.spardl_rms_norm_backward(
         *_mat(fn, "dy", dy, shape, dt), *_mat(fn, "sum", sum, shape, dt), _vec(fn, "weight", weight, dim, dt),
         _vec(fn, "rstd", rstd, rows), *_mat(fn, "dsum", dsum, shape, dt), *_mat(fn, "dx", dx, shape, dt),
-        _vec(fn, "dweight", dweight, dim), rows, dim, _type(fn, dy), *_ws(ws), _on(stream, dy)))
+        _vec(fn, "dweight", dweight, dim), rows, dim, _type(fn, dy), *_ws(ws),
+        _on(fn, stream, dy, sum, weight, rstd, dx, dweight, ws, dsum)))
 
 
 # ---------------------------------------------------------------- distillation loss
@@ -164,7 +177,7 @@ def distill_loss(logits, top_idx, top_val, loss, stats, ws, *, temperature: floa
     lists, rows, vocab, top = _lists(fn, logits, top_idx, top_val)
     _check(fn, _lib.spardl_distill_loss(*lists, rows, vocab, top, temperature, _vec(fn, "loss", loss, rows),
                                         _vec(fn, "stats", stats, 2 * rows), _type(fn, logits), *_ws(ws),
-                                        _on(stream, logits)))
+                                        _on(fn, stream, logits, top_idx, top_val, loss, stats, ws)))
 
 
 def distill_backward(logits, top_idx, top_val, stats, dloss, dlogits, *, temperature: float = 1.0, stream=None) -> None:
@@ -174,7 +187,7 @@ def distill_backward(logits, top_idx, top_val, stats, dloss, dlogits, *, tempera
     _check(fn, _lib.spardl_distill_backward(*lists, _vec(fn, "stats", stats, 2 * rows),
                                             _vec(fn, "dloss", dloss, rows), rows, vocab, top, temperature,
                                             *_mat(fn, "dlogits", dlogits, logits.shape, logits.dtype), _type(fn, logits),
-                                            _on(stream, logits)))
+                                            _on(fn, stream, logits, top_idx, top_val, stats, dloss, dlogits)))
 
 
 def distill_loss_backward(logits, top_idx, top_val, dloss, loss, stats, dlogits, ws, *, temperature: float = 1.0,
@@ -185,7 +198,8 @@ def distill_loss_backward(logits, top_idx, top_val, dloss, loss, stats, dlogits,
     _check(fn, _lib.spardl_distill_loss_backward(
         *lists, _vec(fn, "dloss", dloss, rows), rows, vocab, top, temperature,
         _vec(fn, "loss", loss, rows), _vec(fn, "stats", stats, 2 * rows),
-        *_mat(fn, "dlogits", dlogits, logits.shape, logits.dtype), _type(fn, logits), *_ws(ws), _on(stream, logits)))
+        *_mat(fn, "dlogits", dlogits, logits.shape, logits.dtype), _type(fn, logits), *_ws(ws),
+        _on(fn, stream, logits, top_idx, top_val, dloss, loss, stats, dlogits, ws)))
 
 
 # ---------------------------------------------------------------- gated feed-forward block
@@ -222,7 +236,7 @@ def gated_ffn(x, w_gate, w_up, w_down, y, ws, *, gate=None, up=None, act: str = 
         *_mat(fn, "x", x, (rows, dim), dt), *_mat(fn, "w_gate", w_gate, (hidden, dim), dt),
         *_mat(fn, "w_up", w_up, (hidden, dim), dt), *_mat(fn, "w_down", w_down, (dim, hidden), dt),
         *_mat(fn, "y", y, (rows, dim), dt), *_gate_up(fn, gate, up, rows, hidden, dt), rows, dim, hidden, _act(fn, act),
-        _type(fn, x), *_ws(ws), _on(stream, x)))
+        _type(fn, x), *_ws(ws), _on(fn, stream, x, w_gate, w_up, w_down, y, ws, gate, up)))
 
 
 def gated_ffn_backward(dy, x, gate, up, w_gate, w_up, w_down, dx, dw_gate, dw_up, dw_down, ws, *, act: str = "silu",
@@ -236,4 +250,5 @@ def gated_ffn_backward(dy, x, gate, up, w_gate, w_up, w_down, dx, dw_gate, dw_up
         *_mat(fn, "w_up", w_up, (hidden, dim), dt), *_mat(fn, "w_down", w_down, (dim, hidden), dt),
         *_mat(fn, "dx", dx, (rows, dim), dt), *_mat(fn, "dw_gate", dw_gate, (hidden, dim), dwt),
         *_mat(fn, "dw_up", dw_up, (hidden, dim), dwt), *_mat(fn, "dw_down", dw_down, (dim, hidden), dwt),
-        _type(fn, dw_gate), accumulate, rows, dim, hidden, _act(fn, act), _type(fn, x), *_ws(ws), _on(stream, x)))
+        _type(fn, dw_gate), accumulate, rows, dim, hidden, _act(fn, act), _type(fn, x), *_ws(ws),
+        _on(fn, stream, dy, x, gate, up, w_gate, w_up, w_down, dx, dw_gate, dw_up, dw_down, ws)))

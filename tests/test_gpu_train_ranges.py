@@ -11,6 +11,7 @@ import torch
 from paper_2304_00737_amd import train
 from tests import train_ref as ref
 from tests.gpu_util import log
+from tests.train_calls import calls
 
 pytestmark = pytest.mark.gpu
 
@@ -23,6 +24,24 @@ def _gen(*key):
 
 def _randn(g, *shape):
     return torch.randn(*shape, generator=g, device=DEV)
+
+
+# ------------------------------------------------------------------ devices
+
+def test_tensors_off_the_current_device_are_refused(monkeypatch):
+    """Each argument in turn on the host; and all of them on a device that is not the current one."""
+    for name, tensors in calls(DEV):
+        call = getattr(train, name)
+        call(**tensors)
+        for arg, t in tensors.items():
+            with pytest.raises(train.SpardlError, match="current GPU") as err:
+                call(**{**tensors, arg: t.cpu()})
+            assert err.value.status == -1
+    monkeypatch.setattr(train, "_current_device", lambda: 1)
+    for name, tensors in calls(DEV):
+        for stream in (None, torch.cuda.current_stream()):
+            with pytest.raises(train.SpardlError, match="current GPU"):
+                getattr(train, name)(**tensors, stream=stream)
 
 
 # ------------------------------------------------------------------ distillation

@@ -11,6 +11,7 @@ import subprocess
 import pytest
 
 from tests.test_codegen import CSRC, HIPCC, suspicious_selects
+from tests.train_calls import calls
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 LIB = os.path.join(ROOT, "paper_2304_00737_amd", "libspardl_train.so")
@@ -157,6 +158,17 @@ def test_python_refusals():
     with pytest.raises(train.SpardlError) as err:
         train.gated_ffn(e(2, 8), e(4, 8), e(4, 8), e(8, 4), e(2, 8), e(256), stream=0)    # fp32
     assert err.value.status == EINVAL
+
+
+@needs_lib
+def test_host_tensors_are_refused():
+    """A host tensor's pointer never reaches a kernel; the shapes, types and sizes are all as they should be."""
+    train, _ = _binding()
+    for name, tensors in calls("cpu"):
+        for stream in (None, 0):
+            with pytest.raises(train.SpardlError, match="current GPU") as err:
+                getattr(train, name)(**tensors, stream=stream)
+            assert err.value.status == EINVAL
 
 
 @pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not available")
