@@ -90,6 +90,10 @@ def _ptr(t) -> int:
         return None
     if isinstance(t, int):
         return t
+    if not t.is_cuda:
+        e = SpardlError("tensor", EINVAL)
+        e.args = (f"{e.args[0]}: a device buffer must be on a GPU, is on {t.device}",)
+        raise e
     return t.data_ptr()
 
 

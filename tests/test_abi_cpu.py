@@ -314,3 +314,22 @@ def test_collect_in_add_query():
     assert q(1, 32, R, 10) == 0 and q(1, 32, R - 1, 10) == 1 and q(2, 32, R - 1, 10) == 0
     assert q(8, 8, M, M // 512) == 0 and q(8, 8, M, M // 512 + 1) == 1
     assert q(0, 4, 100, 3) == q(5, 4, 100, 3) == q(1, 4, 3, 1) == q(1, 4, 100, 26) == -1
+
+
+def test_host_tensors_are_refused():
+    """The Python binding hands no host tensor's pointer to a kernel."""
+    import torch
+    from paper_2304_00737_amd import spardl
+    P, n, kb = 4, 1000, 10
+    f = lambda *s: torch.zeros(*s)
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)
+    ws = torch.zeros(1 << 20, dtype=torch.uint8)
+    for call in (lambda: spardl.workspace_init(ws, P, P, n, kb, stream=0),
+                 lambda: spardl.residual_add(f(P, n), f(P, n), P, n, stream=0),
+                 lambda: spardl.block_topk(f(P, n), P, n, P, kb, i(P, P, kb), f(P, P, kb), None, ws, stream=0),
+                 lambda: spardl.sparse_merge_topk(i(P, P, kb), f(P, P, kb), P, n, kb, 1, i(P, 2, kb), f(P, 2, kb), i(P, 2),
+                                                  ws, stream=0),
+                 lambda: spardl.allgather_densify(i(P, P, kb), f(P, P, kb), P, n, kb, f(n), stream=0)):
+        with pytest.raises(spardl.SpardlError, match="must be on a GPU") as err:
+            call()
+        assert err.value.status == spardl.EINVAL
