@@ -95,8 +95,12 @@ def _vec(fn: str, name: str, t, n: int, dtype=torch.float32):
     _refuse(fn, f"{name} must be {n} contiguous elements of {dtype}, is {list(t.shape)} of {t.dtype}")
 
 
-def _ws(ws):
-    return (None, 0) if ws is None else (ws.data_ptr(), ws.numel() * ws.element_size())
+def _ws(fn: str, ws):
+    if ws is None:
+        return None, 0
+    if not ws.is_contiguous():
+        _refuse(fn, f"the workspace must be contiguous, has strides {ws.stride()}")
+    return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
 # the current device and its stream's handle by the shortest way: small calls are bound by what precedes their launch
@@ -149,7 +153,7 @@ def rms_norm_backward(dy, sum, weight, rstd, dx, dweight, ws, dsum=None, *, stre
     _check(fn, _lib.spardl_rms_norm_backward(
         *_mat(fn, "dy", dy, shape, dt), *_mat(fn, "sum", sum, shape, dt), _vec(fn, "weight", weight, dim, dt),
         _vec(fn, "rstd", rstd, rows), *_mat(fn, "dsum", dsum, shape, dt), *_mat(fn, "dx", dx, shape, dt),
-        _vec(fn, "dweight", dweight, dim), rows, dim, _type(fn, dy), *_ws(ws),
+        _vec(fn, "dweight", dweight, dim), rows, dim, _type(fn, dy), *_ws(fn, ws),
         _on(fn, stream, dy, sum, weight, rstd, dx, dweight, ws, dsum)))
 
 
@@ -176,7 +180,7 @@ def distill_loss(logits, top_idx, top_val, loss, stats, ws, *, temperature: floa
     fn = "distill_loss"
     lists, rows, vocab, top = _lists(fn, logits, top_idx, top_val)
     _check(fn, _lib.spardl_distill_loss(*lists, rows, vocab, top, temperature, _vec(fn, "loss", loss, rows),
-                                        _vec(fn, "stats", stats, 2 * rows), _type(fn, logits), *_ws(ws),
+                                        _vec(fn, "stats", stats, 2 * rows), _type(fn, logits), *_ws(fn, ws),
                                         _on(fn, stream, logits, top_idx, top_val, loss, stats, ws)))
 
 
@@ -198,7 +202,7 @@ def distill_loss_backward(logits, top_idx, top_val, dloss, loss, stats, dlogits,
     _check(fn, _lib.spardl_distill_loss_backward(
         *lists, _vec(fn, "dloss", dloss, rows), rows, vocab, top, temperature,
         _vec(fn, "loss", loss, rows), _vec(fn, "stats", stats, 2 * rows),
-        *_mat(fn, "dlogits", dlogits, logits.shape, logits.dtype), _type(fn, logits), *_ws(ws),
+        *_mat(fn, "dlogits", dlogits, logits.shape, logits.dtype), _type(fn, logits), *_ws(fn, ws),
         _on(fn, stream, logits, top_idx, top_val, dloss, loss, stats, dlogits, ws)))
 
 
@@ -236,7 +240,7 @@ def gated_ffn(x, w_gate, w_up, w_down, y, ws, *, gate=None, up=None, act: str = 
         *_mat(fn, "x", x, (rows, dim), dt), *_mat(fn, "w_gate", w_gate, (hidden, dim), dt),
         *_mat(fn, "w_up", w_up, (hidden, dim), dt), *_mat(fn, "w_down", w_down, (dim, hidden), dt),
         *_mat(fn, "y", y, (rows, dim), dt), *_gate_up(fn, gate, up, rows, hidden, dt), rows, dim, hidden, _act(fn, act),
-        _type(fn, x), *_ws(ws), _on(fn, stream, x, w_gate, w_up, w_down, y, ws, gate, up)))
+        _type(fn, x), *_ws(fn, ws), _on(fn, stream, x, w_gate, w_up, w_down, y, ws, gate, up)))
 
 
 def gated_ffn_backward(dy, x, gate, up, w_gate, w_up, w_down, dx, dw_gate, dw_up, dw_down, ws, *, act: str = "silu",
@@ -250,5 +254,5 @@ def gated_ffn_backward(dy, x, gate, up, w_gate, w_up, w_down, dx, dw_gate, dw_up
         *_mat(fn, "w_up", w_up, (hidden, dim), dt), *_mat(fn, "w_down", w_down, (dim, hidden), dt),
         *_mat(fn, "dx", dx, (rows, dim), dt), *_mat(fn, "dw_gate", dw_gate, (hidden, dim), dwt),
         *_mat(fn, "dw_up", dw_up, (hidden, dim), dwt), *_mat(fn, "dw_down", dw_down, (dim, hidden), dwt),
-        _type(fn, dw_gate), accumulate, rows, dim, hidden, _act(fn, act), _type(fn, x), *_ws(ws),
+        _type(fn, dw_gate), accumulate, rows, dim, hidden, _act(fn, act), _type(fn, x), *_ws(fn, ws),
         _on(fn, stream, dy, x, gate, up, w_gate, w_up, w_down, dx, dw_gate, dw_up, dw_down, ws)))

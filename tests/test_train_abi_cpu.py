@@ -161,6 +161,18 @@ def test_python_refusals():
 
 
 @needs_lib
+def test_workspaces_with_gaps_are_refused():
+    """A view's elements times their size are not what lies behind its pointer."""
+    train, _ = _binding()
+    for name, tensors in calls("cpu"):
+        if "ws" in tensors:
+            for ws in (tensors["ws"][::2], tensors["ws"][:1].expand(1 << 20)):
+                with pytest.raises(train.SpardlError, match="must be contiguous") as err:
+                    getattr(train, name)(**{**tensors, "ws": ws}, stream=0)
+                assert err.value.status == EINVAL
+
+
+@needs_lib
 def test_host_tensors_are_refused():
     """A host tensor's pointer never reaches a kernel; the shapes, types and sizes are all as they should be."""
     train, _ = _binding()
