@@ -73,6 +73,13 @@ def _type(fn: str, t) -> int:
     return dt
 
 
+def _shape(fn: str, name: str, t):
+    """The two sizes of the matrix that the other arguments are measured by."""
+    if getattr(t, "ndim", 0) != 2:
+        _refuse(fn, f"{name} must be a matrix, is {None if t is None else list(t.shape)}")
+    return t.shape
+
+
 def _mat(fn: str, name: str, t, shape, dtype):
     """(pointer, row distance) of a matrix argument; None is passed on."""
     if t is None:
@@ -133,8 +140,9 @@ def _new_ws(fn: str, nbytes: int, device):
 
 def rms_norm(x, res, weight, sum, y, rstd=None, *, eps: float = 1e-6, stream=None) -> None:
     """sum = x + res, y = sum / rms(sum) * weight; res, sum and rstd may be None."""
-    fn, shape, dt = "rms_norm", x.shape, x.dtype
-    rows, dim = shape
+    fn = "rms_norm"
+    rows, dim = shape = _shape(fn, "x", x)
+    dt = x.dtype
     _check(fn, _lib.spardl_rms_norm(*_mat(fn, "x", x, shape, dt), *_mat(fn, "res", res, shape, dt),
                                     _vec(fn, "weight", weight, dim, dt), *_mat(fn, "sum", sum, shape, dt),
                                     *_mat(fn, "y", y, shape, dt), _vec(fn, "rstd", rstd, rows), rows, dim, eps,
@@ -148,8 +156,9 @@ def rms_norm_workspace(rows: int, dim: int, device="cuda"):
 
 def rms_norm_backward(dy, sum, weight, rstd, dx, dweight, ws, dsum=None, *, stream=None) -> None:
     """dx (of x and of res alike, dsum included) and dweight (float32)."""
-    fn, shape, dt = "rms_norm_backward", dy.shape, dy.dtype
-    rows, dim = shape
+    fn = "rms_norm_backward"
+    rows, dim = shape = _shape(fn, "dy", dy)
+    dt = dy.dtype
     _check(fn, _lib.spardl_rms_norm_backward(
         *_mat(fn, "dy", dy, shape, dt), *_mat(fn, "sum", sum, shape, dt), _vec(fn, "weight", weight, dim, dt),
         _vec(fn, "rstd", rstd, rows), *_mat(fn, "dsum", dsum, shape, dt), *_mat(fn, "dx", dx, shape, dt),
@@ -165,8 +174,8 @@ def distill_workspace(rows: int, vocab: int, device="cuda"):
 
 
 def _lists(fn: str, logits, top_idx, top_val):
-    rows, vocab = logits.shape
-    top = top_idx.shape[-1]
+    rows, vocab = _shape(fn, "logits", logits)
+    top = _shape(fn, "top_idx", top_idx)[1]
     z, ld = _mat(fn, "logits", logits, logits.shape, logits.dtype)
     i, ld_i = _mat(fn, "top_idx", top_idx, (rows, top), torch.int32)
     v, ld_v = _mat(fn, "top_val", top_val, (rows, top), torch.float32)
@@ -235,7 +244,9 @@ def _gate_up(fn: str, gate, up, rows: int, hidden: int, dt):
 
 def gated_ffn(x, w_gate, w_up, w_down, y, ws, *, gate=None, up=None, act: str = "silu", stream=None) -> None:
     """y = (act(x w_gate^T) * (x w_up^T)) w_down^T; gate and up receive the two products for the backward pass."""
-    fn, (rows, dim), hidden, dt = "gated_ffn", x.shape, w_gate.shape[0], x.dtype
+    fn = "gated_ffn"
+    (rows, dim), (hidden, _) = _shape(fn, "x", x), _shape(fn, "w_gate", w_gate)
+    dt = x.dtype
     _check(fn, _lib.spardl_gated_ffn(
         *_mat(fn, "x", x, (rows, dim), dt), *_mat(fn, "w_gate", w_gate, (hidden, dim), dt),
         *_mat(fn, "w_up", w_up, (hidden, dim), dt), *_mat(fn, "w_down", w_down, (dim, hidden), dt),
@@ -247,7 +258,10 @@ def gated_ffn_backward(dy, x, gate, up, w_gate, w_up, w_down, dx, dw_gate, dw_up
                        accumulate: bool = False, stream=None) -> None:
     """dx (may be None) and the weight gradients, in x's type or in float32
     (views of a worker's gradient row, say); accumulate adds to them."""
-    fn, (rows, dim), hidden, dt, dwt = "gated_ffn_backward", x.shape, w_gate.shape[0], x.dtype, dw_gate.dtype
+    fn = "gated_ffn_backward"
+    (rows, dim), (hidden, _) = _shape(fn, "x", x), _shape(fn, "w_gate", w_gate)
+    _shape(fn, "dw_gate", dw_gate)
+    dt, dwt = x.dtype, dw_gate.dtype
     _check(fn, _lib.spardl_gated_ffn_backward(
         *_mat(fn, "dy", dy, (rows, dim), dt), *_mat(fn, "x", x, (rows, dim), dt),
         *_gate_up(fn, gate, up, rows, hidden, dt), *_mat(fn, "w_gate", w_gate, (hidden, dim), dt),
@@ -255,4 +269,4 @@ def gated_ffn_backward(dy, x, gate, up, w_gate, w_up, w_down, dx, dw_gate, dw_up
         *_mat(fn, "dx", dx, (rows, dim), dt), *_mat(fn, "dw_gate", dw_gate, (hidden, dim), dwt),
         *_mat(fn, "dw_up", dw_up, (hidden, dim), dwt), *_mat(fn, "dw_down", dw_down, (dim, hidden), dwt),
         _type(fn, dw_gate), accumulate, rows, dim, hidden, _act(fn, act), _type(fn, x), *_ws(fn, ws),
-        _on(fn, stream, dy, x, gate, up, w_gate, w_up, w_down, dx, dw_gate, dw_up, dw_down, ws)))
+        _on(fn, stream, x, dy, gate, up, w_gate, w_up, w_down, dx, dw_gate, dw_up, dw_down, ws)))

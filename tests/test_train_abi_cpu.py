@@ -21,6 +21,7 @@ EINVAL, ECAP, OK = -1, -2, 0
 needs_lib = pytest.mark.skipif(not os.path.exists(LIB), reason="libspardl_train.so not built")
 P = 0x1000                      # never dereferenced: validation fails first, or there are no rows
 BIG = 1 << 40
+OPTIONAL = {"res", "sum", "dsum", "dx", "gate", "up"}      # None by themselves, in some of the calls
 
 
 def _binding():
@@ -170,6 +171,19 @@ def test_workspaces_with_gaps_are_refused():
                 with pytest.raises(train.SpardlError, match="must be contiguous") as err:
                     getattr(train, name)(**{**tensors, "ws": ws}, stream=0)
                 assert err.value.status == EINVAL
+
+
+@needs_lib
+def test_arguments_that_are_no_matrices_are_refused():
+    """Missing, one-dimensional and three-dimensional arguments: an error of this library, whichever they are."""
+    train, _ = _binding()
+    for name, tensors in calls("cpu"):
+        for arg, t in tensors.items():
+            if t.ndim == 2:
+                for other in (None, t[0], t[None]) if arg not in OPTIONAL else (t[0], t[None]):
+                    with pytest.raises(train.SpardlError) as err:
+                        getattr(train, name)(**{**tensors, arg: other}, stream=0)
+                    assert err.value.status == EINVAL, (name, arg)
 
 
 @needs_lib
