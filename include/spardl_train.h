@@ -117,7 +117,8 @@ int spardl_distill_loss_backward(const void* logits, int64_t ld, const int32_t* 
  * workspace_bytes: backward != 0 for the backward pass (which needs more);
  * unaligned != 0 if a row of x, dy or a weight may start at an address that
  * is not a multiple of 16 bytes (an odd dim or hidden, a view): the products
- * then work on aligned copies in ws.  0 on invalid sizes.
+ * then work on aligned copies in ws.  0 on invalid sizes.  The bytes never fall
+ * as tokens grow: the largest batch's workspace serves every smaller one.
  * Errors: EINVAL for NULL x, weights or y, one of gate and up without the
  * other, tokens < 0 or >= 2^31, dim or hidden outside [1, 2^20], a product of
  * two of them past 2^36, ld below the row's length, an unknown act, a dtype

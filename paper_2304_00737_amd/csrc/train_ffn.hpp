@@ -75,6 +75,27 @@ struct Plan {
   int64_t floats;      // of partial sums; 0: none
 };
 
+inline int64_t round_of(int tile) { return tile == 256 ? 256 : 512; }      // tiles that the card holds at once
+template <Epi E>
+int columns(int tile) { return E == Epi::Gate ? tile / 2 : tile; }         // of the product, in a tile
+
+// A launch's tiles, the K steps of its longest product and the values of its results.
+struct Extent {
+  int64_t tiles, steps, values;
+};
+template <Epi E>
+Extent extent(const Gemm& g, int tile) {
+  Extent x = {};
+  for (int i = 0; i < g.products; ++i) {
+    const Product& p = g.p[i];
+    x.tiles += ceil_div(p.M, tile) * ceil_div(p.pad_n, columns<E>(tile));
+    x.values += (int64_t)p.M * p.pad_n * (E == Epi::Gate ? 2 : 1);
+    const int64_t s = ceil_div(p.K, KSTEP) * p.segments;
+    x.steps = x.steps > s ? x.steps : s;
+  }
+  return x;
+}
+
 // The plan of least estimated time, in us, from what was measured on products
 // of 64 .. 8192 x 1600 .. 11008: a step of a tile of 256 (one workgroup a CU)
 // takes 1.65, of tiles of 128 1.0 with two on a CU and alone 0.5 if both
@@ -84,19 +105,11 @@ struct Plan {
 // matrices; joining cut tiles 5 and their bytes, read and written at 5e6 a us.
 template <Epi E, bool ALONG>
 Plan plan(Gemm& g) {
-  constexpr bool DUAL = E == Epi::Gate;
   Plan best = {0, 0, 1, 0};
   double least = 0;
   for (int tile = 128; tile <= 256; tile += 128) {
-    int64_t tiles = 0, steps = 0, values = 0;
-    for (int i = 0; i < g.products; ++i) {
-      const Product& p = g.p[i];
-      tiles += ceil_div(p.M, tile) * ceil_div(p.pad_n, DUAL ? tile / 2 : tile);
-      values += (int64_t)p.M * p.pad_n * (DUAL ? 2 : 1);
-      const int64_t s = ceil_div(p.K, KSTEP) * p.segments;
-      steps = steps > s ? steps : s;
-    }
-    const int64_t slots = tile == 256 ? 256 : 512, full = tiles / slots, rest = tiles % slots;
+    const auto [tiles, steps, values] = extent<E>(g, tile);
+    const int64_t slots = round_of(tile), full = tiles / slots, rest = tiles % slots;
     const bool big = tile == 256;
     const double step = big ? 1.65 : 1.0;
     const double ends = (big ? 6.0 : 4.0) + (E == Epi::GateBackward ? big ? 25.0 : 9.0 : 0.0);
@@ -118,11 +131,27 @@ Plan plan(Gemm& g) {
   for (int i = 0; i < g.products; ++i) {
     Product& p = g.p[i];
     p.tiles_m = (int32_t)ceil_div(p.M, best.tile);
-    p.tiles_n = (int32_t)ceil_div(p.pad_n, DUAL ? best.tile / 2 : best.tile);
+    p.tiles_n = (int32_t)ceil_div(p.pad_n, columns<E>(best.tile));
     p.first = g.tiles;
     g.tiles += p.tiles_m * p.tiles_n;
   }
   return best;
+}
+
+// Floats of partial sums that no plan passes, for these products or smaller
+// ones: all runs of the cut tiles fit a round of the card, and a run is four
+// steps at least.  A plan's own need falls where one more tile ends a round, so
+// a workspace sized by it would not serve a shorter batch.
+template <Epi E>
+int64_t most_partials(const Gemm& g) {
+  int64_t most = 0;
+  for (int tile = 128; tile <= 256; tile += 128) {
+    const Extent x = extent<E>(g, tile);
+    const int64_t splits = x.steps / 4, runs = x.tiles * splits < round_of(tile) ? x.tiles * splits : round_of(tile);
+    const int64_t floats = splits > 1 ? runs * tile * tile : 0;
+    most = most > floats ? most : floats;
+  }
+  return most;
 }
 
 template <typename T, bool M_ALONG, bool N_ALONG, Epi E>

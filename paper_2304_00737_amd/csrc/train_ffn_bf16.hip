@@ -23,20 +23,20 @@ size_t gated_ffn_ws(int64_t tokens, int32_t dim, int32_t hidden, bool backward, 
   if (!backward) {
     one(T, hidden, dim, 1);
     g.p[0].pad_n = (int32_t)Fp;
-    see(plan<Epi::Gate, true>(g).floats);
+    see(most_partials<Epi::Gate>(g));
     one(T, dim, hidden, 1);
-    see(plan<Epi::Store, true>(g).floats);
+    see(most_partials<Epi::Store>(g));
   } else {
     one(T, hidden, dim, 1);
     g.p[0].pad_n = (int32_t)Fp;
-    see(plan<Epi::GateBackward, false>(g).floats);
+    see(most_partials<Epi::GateBackward>(g));
     one(T, dim, hidden, 2);
-    see(plan<Epi::Store, false>(g).floats);
+    see(most_partials<Epi::Store>(g));
     if (T > kOuterTokens) {
       g.products = 3;
       g.p[0] = g.p[1] = product({}, {}, hidden, dim, T);
       g.p[2] = product({}, {}, dim, hidden, T);
-      see(plan<Epi::Store, false>(g).floats);
+      see(most_partials<Epi::Store>(g));
     }
   }
   return b + align256((size_t)most * 4) + 256;

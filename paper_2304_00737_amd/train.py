@@ -219,7 +219,7 @@ def distill_loss_backward(logits, top_idx, top_val, dloss, loss, stats, dlogits,
 
 def gated_ffn_workspace(tokens: int, dim: int, hidden: int, dtype=torch.bfloat16, *, backward: bool = False,
                         unaligned: bool = False, device="cuda"):
-    """Scratch for gated_ffn, with backward=True for gated_ffn_backward too.
+    """Scratch for gated_ffn of up to `tokens` tokens, with backward=True for gated_ffn_backward too.
     unaligned: a row of x, dy or a weight may start off a 16-byte boundary
     though dim and hidden are multiples of 8 (a view)."""
     if dtype not in (torch.bfloat16, torch.float16):

@@ -44,6 +44,38 @@ def test_tensors_off_the_current_device_are_refused(monkeypatch):
                 getattr(train, name)(**tensors, stream=stream)
 
 
+# ------------------------------------------------------------------ a workspace for the largest batch
+
+def _in_front(nbytes, most):
+    """A workspace of nbytes, and a check that the bytes behind it, up to what `most` more would take, still stand."""
+    whole = torch.full((nbytes + most,), 0xA5, dtype=torch.uint8, device=DEV)
+    return whole[:nbytes], lambda: bool((whole[nbytes:] == 0xA5).all())
+
+
+@pytest.mark.parametrize("batch,dim,hidden,smaller", [(2560, 1600, 6400, (2304, 1536, 1534, 649)),
+                                                      (2048, 1001, 2731, (1920, 777, 124)), (1290, 256, 704, (1280,)),
+                                                      (512, 256, 704, (200,))])
+def test_ffn_smaller_batches_in_the_workspace(batch, dim, hidden, smaller):
+    """Forward and backward each in its largest batch's workspace: as in one of their own, which they do not leave."""
+    dt = torch.bfloat16
+    g = _gen("last batch", batch, dim)
+    dy, x = (_randn(g, batch, dim).to(dt) for _ in range(2))
+    gate, up = (torch.empty(batch, hidden, dtype=dt, device=DEV) for _ in range(2))
+    wg, wu, wd = (_randn(g, *s).to(dt) for s in ((hidden, dim), (hidden, dim), (dim, hidden)))
+    shared = [train.gated_ffn_workspace(batch, dim, hidden, dt), train.gated_ffn_workspace(batch, dim, hidden, dt, backward=True)]
+    for tokens in (batch, *smaller, 130, 33, 32, 17, 16, 1):
+        log(f"ffn workspace {tokens} of {batch} x {dim} x {hidden}")
+        own = [_in_front(train.gated_ffn_workspace(tokens, dim, hidden, dt, backward=b).numel(), 1 << 20) for b in (False, True)]
+        results = []
+        for first, second in (shared, [ws for ws, _ in own]):
+            y, dx = torch.empty(tokens, dim, dtype=dt, device=DEV), torch.empty(tokens, dim, dtype=dt, device=DEV)
+            grads = [torch.empty_like(w) for w in (wg, wu, wd)]
+            train.gated_ffn(x[:tokens], wg, wu, wd, y, first, gate=gate[:tokens], up=up[:tokens])
+            train.gated_ffn_backward(dy[:tokens], x[:tokens], gate[:tokens], up[:tokens], wg, wu, wd, dx, *grads, second)
+            results.append([y, dx, *grads])
+        assert all(ok() for _, ok in own) and all(torch.equal(a, b) for a, b in zip(*results))
+
+
 # ------------------------------------------------------------------ distillation
 
 def _check_distill(z, idx, val, dloss, t):

@@ -141,6 +141,19 @@ def test_ffn_refusals():
 
 
 @needs_lib
+@pytest.mark.parametrize("dim,hidden", [(1600, 6400), (4096, 11008), (1001, 2731), (256, 704), (64, 64), (1, 1)])
+def test_ffn_workspace_of_a_batch_serves_smaller_ones(dim, hidden):
+    _, lib = _binding()
+    for backward in (0, 1):
+        for unaligned in (0, 1):
+            last = 0
+            for tokens in [*range(0, 2100), *range(2100, 20000, 7)]:
+                now = lib.spardl_gated_ffn_workspace_bytes(tokens, dim, hidden, backward, unaligned)
+                assert now >= last, (tokens, backward, unaligned, last, now)
+                last = now
+
+
+@needs_lib
 def test_python_refusals():
     import torch
     train, _ = _binding()
