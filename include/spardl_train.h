@@ -21,7 +21,9 @@
  *  - ws is scratch device memory of at least the bytes that the call's
  *    *_workspace_bytes function returns, 256-byte aligned (EINVAL otherwise;
  *    ECAPACITY if it is smaller).  It needs no preparation and holds nothing
- *    between calls.  Calls on different streams must use different ws.
+ *    between calls.  Calls on different streams must use different ws.  The
+ *    bytes never fall as rows or tokens grow: the largest batch's workspace
+ *    serves every smaller one of the same widths.
  *  - Results are deterministic: the same arguments give the same bits.
  *  - Inputs and outputs must not overlap unless a call says so.
  */
@@ -117,8 +119,7 @@ int spardl_distill_loss_backward(const void* logits, int64_t ld, const int32_t* 
  * workspace_bytes: backward != 0 for the backward pass (which needs more);
  * unaligned != 0 if a row of x, dy or a weight may start at an address that
  * is not a multiple of 16 bytes (an odd dim or hidden, a view): the products
- * then work on aligned copies in ws.  0 on invalid sizes.  The bytes never fall
- * as tokens grow: the largest batch's workspace serves every smaller one.
+ * then work on aligned copies in ws.  0 on invalid sizes.
  * Errors: EINVAL for NULL x, weights or y, one of gate and up without the
  * other, tokens < 0 or >= 2^31, dim or hidden outside [1, 2^20], a product of
  * two of them past 2^36, ld below the row's length, an unknown act, a dtype

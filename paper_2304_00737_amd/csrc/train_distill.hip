@@ -406,7 +406,10 @@ hipError_t launch(const Distill& d, void* ws, hipStream_t s) {
 }  // namespace
 
 size_t distill_ws(int64_t rows, int32_t vocab) {
-  return align256((size_t)((rows < 1 ? 1 : rows) * segments(rows, vocab)) * sizeof(Running));
+  // For any number of rows up to these: r rows take r segments(r) parts, at most r + kFill - 1 of them and
+  // at most as many as rows of segments of kSegMin have.
+  const int64_t most = (rows < 1 ? 1 : rows) * ceil_div(vocab, kSegMin), parts = rows + kFill - 1;
+  return align256((size_t)(parts < most ? parts : most) * sizeof(Running));
 }
 
 hipError_t launch_distill(const Distill& d, void* ws, hipStream_t s) {

@@ -169,7 +169,7 @@ def rms_norm_backward(dy, sum, weight, rstd, dx, dweight, ws, dsum=None, *, stre
 # ---------------------------------------------------------------- distillation loss
 
 def distill_workspace(rows: int, vocab: int, device="cuda"):
-    """Scratch for distill_loss and distill_loss_backward of these sizes."""
+    """Scratch for distill_loss and distill_loss_backward over up to `rows` rows of vocab logits."""
     return _new_ws("distill_workspace_bytes", _lib.spardl_distill_workspace_bytes(rows, vocab), device)
 
 

@@ -76,6 +76,27 @@ def test_ffn_smaller_batches_in_the_workspace(batch, dim, hidden, smaller):
         assert all(ok() for _, ok in own) and all(torch.equal(a, b) for a, b in zip(*results))
 
 
+def test_distill_fewer_rows_in_the_workspace():
+    """As in a workspace of their own, which they do not leave."""
+    vocab, top = 50257, 5
+    g = _gen("last rows")
+    z = 3 * _randn(g, 1024, vocab)
+    idx = torch.randint(vocab, (1024, top), generator=g, device=DEV).to(torch.int32)
+    val, dloss = _randn(g, 1024, top), torch.rand(1024, generator=g, device=DEV)
+    shared = train.distill_workspace(1024, vocab)
+    for rows in (1024, 1023, 1000, 520, 513, 127, 63, 41, 16, 1):
+        log(f"distill workspace {rows} rows")
+        own, ok = _in_front(train.distill_workspace(rows, vocab).numel(), 1 << 16)
+        results = []
+        for ws in (shared, own):
+            loss, stats, loss2, stats2 = (torch.empty(rows, n, device=DEV) for n in (1, 2, 1, 2))
+            d = torch.empty(rows, vocab, device=DEV)
+            train.distill_loss(z[:rows], idx[:rows], val[:rows], loss, stats, ws)
+            train.distill_loss_backward(z[:rows], idx[:rows], val[:rows], dloss[:rows], loss2, stats2, d, ws)
+            results.append([loss, stats, loss2, stats2, d])
+        assert ok() and all(torch.equal(a, b) for a, b in zip(*results))
+
+
 # ------------------------------------------------------------------ distillation
 
 def _check_distill(z, idx, val, dloss, t):

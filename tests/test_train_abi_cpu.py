@@ -154,6 +154,18 @@ def test_ffn_workspace_of_a_batch_serves_smaller_ones(dim, hidden):
 
 
 @needs_lib
+def test_row_workspaces_of_a_batch_serve_smaller_ones():
+    _, lib = _binding()
+    rows = [*range(0, 3000), *range(3000, 70000, 61)]
+    for vocab in (1, 2048, 2049, 8193, 50257, 131072, 1 << 30):
+        sizes = [lib.spardl_distill_workspace_bytes(r, vocab) for r in rows]
+        assert sizes == sorted(sizes) and sizes[0] > 0, vocab
+    for dim in (1, 64, 1001, 4096, 16384):
+        sizes = [lib.spardl_rms_norm_workspace_bytes(r, dim) for r in rows]
+        assert sizes == sorted(sizes) and sizes[0] > 0, dim
+
+
+@needs_lib
 def test_python_refusals():
     import torch
     train, _ = _binding()
