@@ -117,14 +117,17 @@ int spardl_distill_loss_backward(const void* logits, int64_t ld, const int32_t* 
  * h is computed from the unrounded gate and up and rounded to dtype, as
  * the operand of the second product.
  * workspace_bytes: backward != 0 for the backward pass (which needs more);
- * unaligned != 0 if a row of x, dy or a weight may start at an address that
- * is not a multiple of 16 bytes (an odd dim or hidden, a view): the products
- * then work on aligned copies in ws.  0 on invalid sizes.
+ * unaligned != 0 if dim or hidden is a multiple of 8 and yet a row of that
+ * length of x, dy or a weight may start at an address that is not a multiple
+ * of 16 bytes (a view), or has a row distance of 2^21 elements or more: the
+ * products then work on aligned copies in ws, as they do by themselves for
+ * other dim and hidden (but not for a forward pass of up to 16 tokens, which
+ * reads rows as they are).  0 on invalid sizes.
  * Errors: EINVAL for NULL x, weights or y, one of gate and up without the
  * other, tokens < 0 or >= 2^31, dim or hidden outside [1, 2^20], a product of
  * two of them past 2^36, ld below the row's length, an unknown act, a dtype
  * other than the two, or a NULL or misaligned ws; ECAPACITY (also where
- * unaligned rows meet a workspace without room for copies). */
+ * such views meet a workspace without room for copies, for any tokens). */
 size_t spardl_gated_ffn_workspace_bytes(int64_t tokens, int32_t dim, int32_t hidden, int32_t backward,
                                         int32_t unaligned);
 int spardl_gated_ffn(const void* x, int64_t ld_x, const void* w_gate, int64_t ld_gate, const void* w_up,

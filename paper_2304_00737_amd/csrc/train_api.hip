@@ -107,11 +107,11 @@ int ffn_check(const Ffn& f) {
 }
 
 int ffn_workspace(const Ffn& f, bool backward, const void* ws, size_t ws_bytes) {
-  const bool odd = f.dim % 8 || f.hidden % 8;
-  const bool copies = odd || !rows_aligned(f.x, f.ld_x) || !rows_aligned(f.w_gate, f.ld_gate) ||
-                      !rows_aligned(f.w_up, f.ld_up) || !rows_aligned(f.w_down, f.ld_down) ||
-                      (backward && !rows_aligned(f.dy, f.ld_dy));
-  return workspace_check(ws, ws_bytes, gated_ffn_ws(f.tokens, f.dim, f.hidden, backward, copies));
+  // Widths that are no multiple of 8 have gated_ffn_ws ask for copies by themselves, where copies are made.
+  auto view = [](const void* p, int64_t ld, int32_t cols) { return cols % 8 == 0 && !rows_aligned(p, ld); };
+  const bool views = view(f.x, f.ld_x, f.dim) || view(f.w_gate, f.ld_gate, f.dim) || view(f.w_up, f.ld_up, f.dim) ||
+                     view(f.w_down, f.ld_down, f.hidden) || (backward && view(f.dy, f.ld_dy, f.dim));
+  return workspace_check(ws, ws_bytes, gated_ffn_ws(f.tokens, f.dim, f.hidden, backward, views));
 }
 
 }  // namespace
@@ -155,7 +155,7 @@ int spardl_distill_loss_backward(const void* logits, int64_t ld, const int32_t* 
 size_t spardl_gated_ffn_workspace_bytes(int64_t tokens, int32_t dim, int32_t hidden, int32_t backward,
                                         int32_t unaligned) {
   if (!ffn_sizes(tokens, dim, hidden)) return 0;
-  return gated_ffn_ws(tokens, dim, hidden, backward != 0, unaligned != 0 || dim % 8 || hidden % 8);
+  return gated_ffn_ws(tokens, dim, hidden, backward != 0, unaligned != 0);
 }
 
 int spardl_gated_ffn(const void* x, int64_t ld_x, const void* w_gate, int64_t ld_gate, const void* w_up,

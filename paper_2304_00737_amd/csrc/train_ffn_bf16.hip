@@ -7,10 +7,14 @@ namespace spardl_train {
 size_t gated_ffn_ws(int64_t tokens, int32_t dim, int32_t hidden, bool backward, bool unaligned) {
   const int64_t T = tokens, Dp = round8(dim), Fp = round8(hidden);
   size_t b = (backward ? 3 : 1) * align256((size_t)T * Fp * 2);
-  if (unaligned) {
+  // A few tokens' forward pass takes rows as they are and cuts no tiles.  A view has its room all the same, so
+  // that whether one is taken does not depend on the number of tokens.
+  const bool few = !backward && T <= kFewTokens;
+  if (unaligned || (!few && (dim % 8 || hidden % 8))) {
     b += (backward ? 2 : 1) * align256((size_t)T * Dp * 2);
     b += 2 * align256((size_t)hidden * Dp * 2) + align256((size_t)dim * Fp * 2);
   }
+  if (few) return b + 256;
   // the products' partial sums, one product at a time
   Gemm g = {};
   auto one = [&](int64_t M, int32_t N, int64_t K, int32_t segments) {

@@ -221,7 +221,7 @@ def gated_ffn_workspace(tokens: int, dim: int, hidden: int, dtype=torch.bfloat16
                         unaligned: bool = False, device="cuda"):
     """Scratch for gated_ffn of up to `tokens` tokens, with backward=True for gated_ffn_backward too.
     unaligned: a row of x, dy or a weight may start off a 16-byte boundary
-    though dim and hidden are multiples of 8 (a view)."""
+    though its length is a multiple of 8 (a view), or have a stride of 2^21 or more."""
     if dtype not in (torch.bfloat16, torch.float16):
         _refuse("gated_ffn_workspace_bytes", f"no kernel for {dtype}")
     need = [_lib.spardl_gated_ffn_workspace_bytes(tokens, dim, hidden, b, unaligned) for b in range(1 + backward)]

@@ -76,6 +76,23 @@ def test_ffn_smaller_batches_in_the_workspace(batch, dim, hidden, smaller):
         assert all(ok() for _, ok in own) and all(torch.equal(a, b) for a, b in zip(*results))
 
 
+@pytest.mark.parametrize("tokens", [1, 2, 5, 8, 16])
+def test_ffn_few_tokens_of_odd_widths(tokens):
+    """Rows as they are, in a workspace without room for copies of the weights, which they do not leave."""
+    for dim, hidden in ((1001, 2731), (1000, 2731), (1001, 2736)):
+        log(f"ffn {tokens} x {dim} x {hidden}, no copies")
+        g = _gen("few odd", tokens, dim, hidden)
+        x = _randn(g, tokens, dim).half()
+        wg, wu, wd = ((_randn(g, *s) / math.sqrt(s[1])).half() for s in ((hidden, dim), (hidden, dim), (dim, hidden)))
+        nbytes = train.gated_ffn_workspace(tokens, dim, hidden, torch.float16).numel()
+        ws, ok = _in_front(nbytes, 1 << 20)
+        y = torch.empty_like(x)
+        train.gated_ffn(x, wg, wu, wd, y, ws)
+        want = ref.gated_ffn(x, wg, wu, wd, "silu")
+        ref.assert_within("y", y, want[2], want[5], torch.float16)
+        assert ok() and nbytes < 2 * tokens * (hidden + 8) + 1024
+
+
 def test_distill_fewer_rows_in_the_workspace():
     """As in a workspace of their own, which they do not leave."""
     vocab, top = 50257, 5

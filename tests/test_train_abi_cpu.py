@@ -154,6 +154,16 @@ def test_ffn_workspace_of_a_batch_serves_smaller_ones(dim, hidden):
 
 
 @needs_lib
+def test_few_tokens_need_no_copies_of_odd_weights():
+    _, lib = _binding()
+    size = lib.spardl_gated_ffn_workspace_bytes
+    for tokens in (0, 1, 2, 16):
+        for dim, hidden in ((4097, 11009), (4096, 11009), (4097, 11008), (4096, 11008)):
+            assert size(tokens, dim, hidden, 0, 0) <= 2 * tokens * 11016 + 512
+    assert size(17, 4097, 11009, 0, 0) >= size(1, 4096, 11008, 0, 1) >= 6 * 4096 * 11008     # with copies
+
+
+@needs_lib
 def test_row_workspaces_of_a_batch_serve_smaller_ones():
     _, lib = _binding()
     rows = [*range(0, 3000), *range(3000, 70000, 61)]
