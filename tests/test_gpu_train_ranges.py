@@ -114,6 +114,70 @@ def test_distill_fewer_rows_in_the_workspace():
         assert ok() and all(torch.equal(a, b) for a, b in zip(*results))
 
 
+# ------------------------------------------------------------------ activations
+
+def _activation(g, name):
+    """activation and slope in 64 bits, and what 32 bits may miss of each, relative to their own size: the tails
+    fall with exp(-|g|) and exp(-g^2 / 2), and have to keep their leading digits.
+
+    An exponent of size x is off by 2 x 2^-24 to 3 x 2^-24 (a constant's and two products' roundings), the functions by
+    a unit or two in the last place each, GELU's fitted polynomial by 1.1e-6: doubled, rel.  Where the exponential
+    passes the range of 32 bits it is 0, so nothing below 2^-126 times the factor beside it counts."""
+    if name == "silu":
+        t = torch.sigmoid(g)
+        rel, a, one = (g.abs() + 4) * 2.0 ** -22, g * t, torch.sigmoid(-g)
+        slope, size = t + a * one, t + a.abs() * (one + t)
+    else:
+        t = 0.5 * torch.special.erfc(-g / math.sqrt(2))
+        pdf = g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+        rel, a = (g * g + 20) * 2.0 ** -22, g * t
+        slope, size = t + pdf, t + pdf.abs()
+    rel, least = rel.clamp(max=2.0 ** -8), 2.0 ** -126 * (1 + g.abs())
+    return a, slope, rel * a.abs() + least, rel * size + least
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("T", [1, 2, 8, 16, 40])
+def test_activations_keep_their_tails(T, dtype):
+    """The activation and its slope element by element: weights of single ones hand gates in and h, dgate and dup out.
+    up is the power of two that brings a tail to order one, as far as the type has it."""
+    F = 256
+    D = 2 * F + 64
+    wg, wu, wd = (torch.zeros(*s, dtype=dtype, device=DEV) for s in ((F, D), (F, D), (D, F)))
+    one = torch.arange(F, device=DEV)
+    wg[one, one] = wu[one, F + one] = wd[one, one] = 1
+    far = [0.0, -0.0, 20.0, -20.0, 100.0, -100.0, 3e4, -3e4] + ([] if dtype == torch.float16 else [1e30, -1e30, 3e38, -3e38])
+    gate = torch.linspace(-15, 15, T * F, device=DEV).to(dtype)
+    if T > 1:
+        gate[: 2 * len(far)] = torch.tensor(far + far, device=DEV).to(dtype)
+    gate = gate[torch.randperm(T * F, generator=_gen("gates", T), device=DEV)].view(T, F)
+    dy = torch.zeros(T, D, dtype=dtype, device=DEV)
+    dy[:, :F] = 1                                              # dh = 1
+    dy[torch.arange(T), 2 * F + torch.arange(T)] = 1           # row 2 F + t of dw_down is h of token t
+    for name in ("silu", "gelu"):
+        a, slope, ba, bs = _activation(gate.double(), name)
+        most = 15 if dtype == torch.float16 else 60
+        up = torch.exp2(-torch.log2(a.abs().clamp(min=2.0 ** -most, max=1.0)).floor()).to(dtype)
+        x = torch.cat([gate, up, torch.zeros(T, D - 2 * F, dtype=dtype, device=DEV)], 1)
+        y, dx, g_out, u_out = (torch.empty(T, n, dtype=dtype, device=DEV) for n in (D, D, F, F))
+        grads = [torch.empty(*s, device=DEV) for s in ((F, D), (F, D), (D, F))]
+        ws = train.gated_ffn_workspace(T, D, F, dtype, backward=True)
+        train.gated_ffn(x, wg, wu, wd, y, ws, gate=g_out, up=u_out, act=name)
+        assert torch.equal(g_out, gate) and torch.equal(u_out, up)
+        train.gated_ffn_backward(dy, x, gate, up, wg, wu, wd, dx, *grads, ws, act=name)
+        u = up.double()
+        want, bound = a * u, ba * u + ref.E32 * (a * u).abs()
+        ref.assert_within("h", y[:, :F], want, bound, dtype)
+        ref.assert_within("h, backward", grads[2][2 * F:2 * F + T].to(dtype), want, bound, dtype)
+        ref.assert_within("dup", dx[:, F:2 * F], a, ba, dtype)
+        ref.assert_within("dgate", dx[:, :F], slope * u, bs * u + ref.E32 * (slope * u).abs(), dtype)
+        seen = (want.abs() >= 2.0 ** -14) & (a.abs() > 2.0 ** -100)      # there a lost tail fails
+        assert bool((bound + ref.U[dtype] * want.abs() < want.abs() / 16)[seen].all())
+        low = gate[seen].min().item()
+        # seen as far as 2^-14 / 2^most: |a| = 2^-29 and 2^-74 for GELU
+        assert T == 1 or low <= (-12.5 if name == "silu" else -5.5 if dtype == torch.float16 else -9.5)
+
+
 # ------------------------------------------------------------------ distillation
 
 def _check_distill(z, idx, val, dloss, t):
