@@ -73,11 +73,13 @@ def _type(fn: str, t) -> int:
     return dt
 
 
-def _shape(fn: str, name: str, t):
-    """The two sizes of the matrix that the other arguments are measured by."""
-    if getattr(t, "ndim", 0) != 2:
+def _lead(fn: str, name: str, t):
+    """(its shape, pointer and row distance, type) of the matrix that the other arguments are measured by."""
+    try:
+        _, cols = shape = t.shape
+    except (AttributeError, ValueError):
         _refuse(fn, f"{name} must be a matrix, is {None if t is None else list(t.shape)}")
-    return t.shape
+    return shape, (t.data_ptr(), cols) if t.is_contiguous() else _mat(fn, name, t, shape, t.dtype), t.dtype
 
 
 def _mat(fn: str, name: str, t, shape, dtype):
@@ -107,7 +109,7 @@ def _ws(fn: str, ws):
         return None, 0
     if not ws.is_contiguous():
         _refuse(fn, f"the workspace must be contiguous, has strides {ws.stride()}")
-    return ws.data_ptr(), ws.numel() * ws.element_size()
+    return ws.data_ptr(), ws.nbytes
 
 
 # the current device and its stream's handle by the shortest way: small calls are bound by what precedes their launch
@@ -141,9 +143,9 @@ def _new_ws(fn: str, nbytes: int, device):
 def rms_norm(x, res, weight, sum, y, rstd=None, *, eps: float = 1e-6, stream=None) -> None:
     """sum = x + res, y = sum / rms(sum) * weight; res, sum and rstd may be None."""
     fn = "rms_norm"
-    rows, dim = shape = _shape(fn, "x", x)
-    dt = x.dtype
-    _check(fn, _lib.spardl_rms_norm(*_mat(fn, "x", x, shape, dt), *_mat(fn, "res", res, shape, dt),
+    shape, x_at, dt = _lead(fn, "x", x)
+    rows, dim = shape
+    _check(fn, _lib.spardl_rms_norm(*x_at, *_mat(fn, "res", res, shape, dt),
                                     _vec(fn, "weight", weight, dim, dt), *_mat(fn, "sum", sum, shape, dt),
                                     *_mat(fn, "y", y, shape, dt), _vec(fn, "rstd", rstd, rows), rows, dim, eps,
                                     _type(fn, x), _on(fn, stream, x, res, weight, sum, y, rstd)))
@@ -157,11 +159,11 @@ def rms_norm_workspace(rows: int, dim: int, device="cuda"):
 def rms_norm_backward(dy, sum, weight, rstd, dx, dweight, ws, dsum=None, *, stream=None) -> None:
     """dx (of x and of res alike, dsum included) and dweight (float32)."""
     fn = "rms_norm_backward"
-    rows, dim = shape = _shape(fn, "dy", dy)
-    dt = dy.dtype
+    shape, dy_at, dt = _lead(fn, "dy", dy)
+    rows, dim = shape
     _check(fn, _lib.spardl_rms_norm_backward(
-        *_mat(fn, "dy", dy, shape, dt), *_mat(fn, "sum", sum, shape, dt), _vec(fn, "weight", weight, dim, dt),
-        _vec(fn, "rstd", rstd, rows), *_mat(fn, "dsum", dsum, shape, dt), *_mat(fn, "dx", dx, shape, dt),
+        *dy_at, *_mat(fn, "sum", sum, shape, dt), _vec(fn, "weight", weight, dim, dt), _vec(fn, "rstd", rstd, rows),
+        *_mat(fn, "dsum", dsum, shape, dt), *_mat(fn, "dx", dx, shape, dt),
         _vec(fn, "dweight", dweight, dim), rows, dim, _type(fn, dy), *_ws(fn, ws),
         _on(fn, stream, dy, sum, weight, rstd, dx, dweight, ws, dsum)))
 
@@ -174,14 +176,14 @@ def distill_workspace(rows: int, vocab: int, device="cuda"):
 
 
 def _lists(fn: str, logits, top_idx, top_val):
-    rows, vocab = _shape(fn, "logits", logits)
-    top = _shape(fn, "top_idx", top_idx)[1]
-    z, ld = _mat(fn, "logits", logits, logits.shape, logits.dtype)
-    i, ld_i = _mat(fn, "top_idx", top_idx, (rows, top), torch.int32)
-    v, ld_v = _mat(fn, "top_val", top_val, (rows, top), torch.float32)
+    (rows, vocab), (z, ld), _ = _lead(fn, "logits", logits)
+    shape, (i, ld_i), dt = _lead(fn, "top_idx", top_idx)
+    if shape[0] != rows or dt is not torch.int32:
+        _mat(fn, "top_idx", top_idx, (rows, shape[1]), torch.int32)     # refuses
+    v, ld_v = _mat(fn, "top_val", top_val, shape, torch.float32)
     if ld_i != ld_v:
         _refuse(fn, "top_idx and top_val must have one row stride")
-    return (z, ld, i, v, ld_i), rows, vocab, top
+    return (z, ld, i, v, ld_i), rows, vocab, shape[1]
 
 
 def distill_loss(logits, top_idx, top_val, loss, stats, ws, *, temperature: float = 1.0, stream=None) -> None:
@@ -199,7 +201,8 @@ def distill_backward(logits, top_idx, top_val, stats, dloss, dlogits, *, tempera
     lists, rows, vocab, top = _lists(fn, logits, top_idx, top_val)
     _check(fn, _lib.spardl_distill_backward(*lists, _vec(fn, "stats", stats, 2 * rows),
                                             _vec(fn, "dloss", dloss, rows), rows, vocab, top, temperature,
-                                            *_mat(fn, "dlogits", dlogits, logits.shape, logits.dtype), _type(fn, logits),
+                                            *_mat(fn, "dlogits", dlogits, logits.shape, logits.dtype),
+                                            _type(fn, logits),
                                             _on(fn, stream, logits, top_idx, top_val, stats, dloss, dlogits)))
 
 
@@ -245,10 +248,10 @@ def _gate_up(fn: str, gate, up, rows: int, hidden: int, dt):
 def gated_ffn(x, w_gate, w_up, w_down, y, ws, *, gate=None, up=None, act: str = "silu", stream=None) -> None:
     """y = (act(x w_gate^T) * (x w_up^T)) w_down^T; gate and up receive the two products for the backward pass."""
     fn = "gated_ffn"
-    (rows, dim), (hidden, _) = _shape(fn, "x", x), _shape(fn, "w_gate", w_gate)
-    dt = x.dtype
+    (rows, dim), x_at, dt = _lead(fn, "x", x)
+    hidden = _lead(fn, "w_gate", w_gate)[0][0]
     _check(fn, _lib.spardl_gated_ffn(
-        *_mat(fn, "x", x, (rows, dim), dt), *_mat(fn, "w_gate", w_gate, (hidden, dim), dt),
+        *x_at, *_mat(fn, "w_gate", w_gate, (hidden, dim), dt),
         *_mat(fn, "w_up", w_up, (hidden, dim), dt), *_mat(fn, "w_down", w_down, (dim, hidden), dt),
         *_mat(fn, "y", y, (rows, dim), dt), *_gate_up(fn, gate, up, rows, hidden, dt), rows, dim, hidden, _act(fn, act),
         _type(fn, x), *_ws(fn, ws), _on(fn, stream, x, w_gate, w_up, w_down, y, ws, gate, up)))
@@ -259,12 +262,12 @@ def gated_ffn_backward(dy, x, gate, up, w_gate, w_up, w_down, dx, dw_gate, dw_up
     """dx (may be None) and the weight gradients, in x's type or in float32
     (views of a worker's gradient row, say); accumulate adds to them."""
     fn = "gated_ffn_backward"
-    (rows, dim), (hidden, _) = _shape(fn, "x", x), _shape(fn, "w_gate", w_gate)
-    _shape(fn, "dw_gate", dw_gate)
-    dt, dwt = x.dtype, dw_gate.dtype
+    (rows, dim), x_at, dt = _lead(fn, "x", x)
+    hidden = _lead(fn, "w_gate", w_gate)[0][0]
+    dwt = _lead(fn, "dw_gate", dw_gate)[2]
     _check(fn, _lib.spardl_gated_ffn_backward(
-        *_mat(fn, "dy", dy, (rows, dim), dt), *_mat(fn, "x", x, (rows, dim), dt),
-        *_gate_up(fn, gate, up, rows, hidden, dt), *_mat(fn, "w_gate", w_gate, (hidden, dim), dt),
+        *_mat(fn, "dy", dy, (rows, dim), dt), *x_at, *_gate_up(fn, gate, up, rows, hidden, dt),
+        *_mat(fn, "w_gate", w_gate, (hidden, dim), dt),
         *_mat(fn, "w_up", w_up, (hidden, dim), dt), *_mat(fn, "w_down", w_down, (dim, hidden), dt),
         *_mat(fn, "dx", dx, (rows, dim), dt), *_mat(fn, "dw_gate", dw_gate, (hidden, dim), dwt),
         *_mat(fn, "dw_up", dw_up, (hidden, dim), dwt), *_mat(fn, "dw_down", dw_down, (dim, hidden), dwt),
