@@ -114,6 +114,40 @@ def test_distill_fewer_rows_in_the_workspace():
         assert ok() and all(torch.equal(a, b) for a, b in zip(*results))
 
 
+# ------------------------------------------------------------------ offsets
+
+@pytest.mark.parametrize("T", [1, 2, 5, 16, 20, 40])
+def test_ffn_offsets_past_32_bits(T):
+    """Every matrix in rows 2^28 + 8 elements apart: views of one allocation, beside each other."""
+    D, F, dt, pitch = 40, 24, torch.bfloat16, (1 << 28) + 8
+    g = _gen("far", T)
+    far = {dt: torch.empty(40 * pitch, dtype=dt, device=DEV), torch.float32: torch.empty(40 * pitch, device=DEV)}
+    used = {dt: 0, torch.float32: 0}
+
+    def view(rows, cols, dtype=dt):
+        at, used[dtype] = used[dtype], used[dtype] + cols + 3
+        return far[dtype].as_strided((rows, cols), (pitch, 1), at)
+
+    names = ("dy", "x", "wg", "wu", "wd")
+    plain = dict(zip(names, ((_randn(g, *s) / math.sqrt(s[1])).to(dt) for s in ((T, D), (T, D), (F, D), (F, D), (D, F)))))
+    v = {}
+    for k, t in plain.items():
+        v[k] = view(*t.shape)
+        v[k].copy_(t)
+    gate, up, y, dx = view(T, F), view(T, F), view(T, D), view(T, D)
+    grads = [view(*s, torch.float32) for s in ((F, D), (F, D), (D, F))]
+    ws = train.gated_ffn_workspace(T, D, F, dt, backward=True, unaligned=True)
+    log(f"ffn far rows, {T} tokens")
+    train.gated_ffn(v["x"], v["wg"], v["wu"], v["wd"], y, ws, gate=gate, up=up)
+    want = ref.gated_ffn(*(plain[k] for k in names[1:]), "silu")
+    for got, w, b in zip((gate, up, y), want[:3], want[3:]):
+        ref.assert_within("forward", got, w, b, dt)
+    train.gated_ffn_backward(v["dy"], v["x"], gate, up, v["wg"], v["wu"], v["wd"], dx, *grads, ws)
+    want, bounds = ref.gated_ffn_backward(plain["dy"], plain["x"], gate, up, *(plain[k] for k in names[2:]), "silu")
+    for got, w, b in zip((dx, *grads), want, bounds):
+        ref.assert_within("backward", got, w, b, got.dtype)
+
+
 # ------------------------------------------------------------------ activations
 
 def _activation(g, name):
