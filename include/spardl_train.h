@@ -50,7 +50,8 @@ enum { SPARDL_ACT_SILU = 0, SPARDL_ACT_GELU = 1 };
 /* Residual RMS norm.  For every row r < rows, with s = x[r] + res[r]:
  *   sum[r] = s,   rstd[r] = 1 / sqrt(mean(s^2) + eps),
  *   y[r]   = s * rstd[r] * weight.
- * y is computed from the unrounded s.  res may be NULL (s = x); sum may be
+ * y is computed from the unrounded s.  The squares and their sum are fp32: a row
+ * of |s| past about 2^63 has rstd = 0.  res may be NULL (s = x); sum may be
  * NULL, or x or res itself (with its ld).  rstd may be NULL.
  * Errors: EINVAL for NULL x, weight or y, rows < 0, dim outside
  * [1, SPARDL_NORM_MAX_DIM], ld < dim, eps not >= 0, an unknown dtype. */
@@ -114,8 +115,8 @@ int spardl_distill_loss_backward(const void* logits, int64_t ld, const int32_t* 
  * with w_gate and w_up [hidden, dim] and w_down [dim, hidden] (w_gate and
  * w_up may be halves of one matrix).  gate and up receive what the backward
  * pass needs, with one row distance ld_hidden; both may be NULL (inference).
- * h is computed from the unrounded gate and up and rounded to dtype, as
- * the operand of the second product.
+ * h is computed from the unrounded gate and up and rounded to dtype, as the
+ * operand of the second product, for any number of tokens.
  * workspace_bytes: backward != 0 for the backward pass (which needs more);
  * unaligned != 0 if dim or hidden is a multiple of 8 and yet a row of that
  * length of x, dy or a weight may start at an address that is not a multiple
@@ -143,7 +144,8 @@ int spardl_gated_ffn(const void* x, int64_t ld_x, const void* w_gate, int64_t ld
  * operands of the products.  The weight gradients have the weights' shapes and are of
  * dw_dtype: dtype, or SPARDL_FP32, so that they can be written straight into
  * a worker's row of a gradient matrix (spardl_residual_add).  With accumulate
- * != 0 they are added to what dw_* holds.  dx may be NULL (not computed).
+ * != 0 they are added to what dw_* holds, in fp32, and rounded to dw_dtype at
+ * every call.  dx may be NULL (not computed).
  * tokens = 0 writes dw_* = 0 (nothing with accumulate).
  * Errors: as spardl_gated_ffn, plus EINVAL for NULL dy, gate, up or dw_*, and
  * a dw_dtype other than dtype and SPARDL_FP32. */

@@ -5,9 +5,12 @@
 // logits of the row's slots only, and the gradient a second look at the row.
 // The logits' bytes bound it: V elements in, and V out for the gradient.
 // With few rows each row is cut into segments, whose (m, s) are joined in
-// order.  4096 x 50257 bf16, loss and gradient: 167 us, 4.9 TB/s; 8192 x 131072
-// 918 us, 4.7 TB/s (its exponentials take half the time of a row, and only
-// partly that of its memory); gradient alone of 1000 x 32003 fp16 27 us.
+// order.  4096 x 50257 bf16, loss and gradient: 167 us, 4.9 TB/s (rows of odd
+// pitch 197; fp32 437, 3.8 TB/s); 8192 x 131072 916 us, 4.7 TB/s (its
+// exponentials take half the time of a row, and only partly that of its
+// memory); gradient alone of 1000 x 32003 fp16 27 us.  The loss alone of 300 and
+// 1000 rows of 50257 bf16 takes 13.5 and 24.8 us for 4.9 and 16.2 of reading:
+// scan_row has about one load a wave under way.
 
 #include "train.hpp"
 
@@ -143,7 +146,10 @@ __device__ bool settle_list(List& L, int top, float t, Running q, bool want_loss
 }
 
 // The list's tokens in [first, end), each from all of its slots, over what a
-// first write put there; a barrier lies between the two.
+// first write put there; a barrier lies between the two.  A token may stand in
+// several slots, so a slot looks at all of them: top^2 reads of LDS a row.  Step
+// of 4096 x 50257 bf16, odd pitch: 197 us with 64 slots, 266 with 256, 1005 with
+// 1024.
 template <typename T, int THREADS>
 __device__ void write_list(const List& L, T* out, int64_t first, int64_t end, int top, float c, Running q, float scale) {
   for (int k = threadIdx.x; k < top; k += THREADS) {
@@ -210,7 +216,9 @@ __global__ __launch_bounds__(THREADS) void k_distill_row(Distill d) {
 }
 
 // The same for a row of at most THREADS x NCH chunks, which stays in the
-// registers of its workgroup between the two looks at it.
+// registers of its workgroup between the two looks at it.  (1024 x 16 in fp16 and
+// fp32 spills 12 registers a lane: 4096 x 131072 fp16 500 us, bf16 465.)  Chunks
+// past the row's end cost their exponentials too: 4096 x 64000 bf16 326 us.
 template <typename T, int THREADS, int NCH, int PER_CU>
 __global__ __launch_bounds__(THREADS, PER_CU * THREADS / 256) void k_distill_held(Distill d) {
   constexpr int N = Chunk<T>::N;

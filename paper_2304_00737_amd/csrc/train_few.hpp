@@ -6,9 +6,13 @@
 // Up to 2 tokens a wave takes whole rows of the weights, 1 KB at a time, and
 // adds in fp32.  Up to 16, 8 or 16 rows a workgroup on MFMA, whose waves take
 // runs of K in turn; their sums meet in LDS, added in the waves' order.  Block
-// of bf16, one token, 4096 x 11008 53 us (5.1 TB/s), 1600 x 6400 17 us (as tiles
+// of bf16, one token, 4096 x 11008 54 us (5.0 TB/s), 1600 x 6400 17 us (as tiles
 // 78 and 37 us); 4 tokens 59 and 20, 16 tokens 76 and 24 us (tiles 79 and 37);
 // 4 tokens by rows, four at a time, 76 us.
+//
+// h is rounded to the type between the products, as it is for more tokens: up to
+// 2 tokens no matrix instruction asks for that, but every row's wave reads h
+// whole, and one token's y does not change its precision with the batch.
 #pragma once
 
 #include "train_gemm.hpp"

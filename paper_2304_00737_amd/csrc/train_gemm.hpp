@@ -17,12 +17,16 @@
 // 8-byte loads (16 lanes take 4 rows x 16 columns and get 4 k of one column
 // each).  The exclusive-or spreads what a wave reads at once over all banks.
 //
-// What bounds it, at 8192 x 4096 x 11008 bf16: h w_down^T takes 590 us (1.25
-// PFLOP/s, matrix cores busy 62 % at 2.0 GHz).  Without its loads it takes 402,
-// with half of them 409, without its LDS reads 579: 64 KB a step and CU from L2
-// into LDS, which alone take 0.5 to 0.6 us of the 1.65 us of a step.  Weight
-// gradients 1.70 ms (1.30), gradient of x 1.07 ms (1.38), gate and up 1.2 ms
-// (1.23), the gate's backward product 0.78 ms (0.94, its epilogue moves 0.9 GB).
+// What bounds it, at 8192 x 4096 x 11008 bf16: h w_down^T takes 600 us (1.23
+// PFLOP/s, matrix cores busy 62 % at 2.0 GHz): 64 KB a step and CU from L2 into
+// LDS, which alone take 0.5 to 0.6 us of the 1.65 us of a step.  (An earlier
+// state of this kernel, in a run of its own: 573 us whole, 402 without its
+// loads, 409 with half of them, 579 without its LDS reads.)  Weight gradients
+// 1.74 ms (1.27), gradient of x 1.11 ms (1.33), gate and up 1.24 ms (1.20), the
+// gate's backward product 0.79 ms (0.94, its epilogue moves 0.9 GB).  A lone
+// tile of 128 on a CU: 6 us of launch, first loads and epilogue, and 0.5 us a
+// step, of which the matrix cores take 0.24 and LDS reads 0.21; its waves wait
+// for 40 % of their time, for LDS 4 to 8 %.
 #pragma once
 
 #include "train.hpp"

@@ -1,7 +1,10 @@
 // The residual RMS norm and its backward pass.  Both stream their rows once:
 // a row lives in the registers of the threads that share it, so the bytes
 // bound them (two rows in and two out forward, three in and one out backward).
-// 16384 x 4096 bf16: forward 89 us, 6.0 TB/s; backward 104 us, 5.2 TB/s.
+// 16384 x 4096 bf16: forward 89 us, 6.0 TB/s; backward 105 us, 5.1 TB/s; fp32 179
+// and 181 us.  Narrow rows do not fill their lanes, since a wave holds one row:
+// 65536 x 256 bf16 (32 of 64 lanes) 32 and 50 us for 22 of bytes, x 64 (8 lanes)
+// 24 and 40 for 5.4.
 
 #include "train.hpp"
 
@@ -76,7 +79,8 @@ __device__ __forceinline__ void store_chunk_f32(float* row, int e0, int dim, con
 // A workgroup walks rows b, b + grid, ..., and keeps its part of dweight in
 // registers; part[b] receives it at the end, a workgroup's rows joined in LDS.  The next row is loaded, packed, while the
 // present one is worked on, where a thread's share of two rows fits its
-// registers (16384 x 4096 bf16: 111 us without, 102 with).
+// registers (16384 x 4096 bf16: 111 us without, 102 with).  fp32 rows past 8192
+// spill 17 registers a lane: 4096 x 16384 206 us for 173 of bytes.
 template <typename T, int THREADS, int NCH>
 __global__ __launch_bounds__(THREADS == 64 ? 256 : THREADS) void k_rms_norm_backward(
     const T* dy, int64_t ld_dy, const T* sum, int64_t ld_sum, const T* weight, const float* rstd, const T* dsum,
