@@ -160,12 +160,7 @@ __global__ __launch_bounds__(512) void k_few(Product p) {
     for (int w = 0; w < W; ++w)
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[w][i] += sums[s][(w * TOKENS + token) * PITCH + col + i];
-  // columns past N took the last row's weights
-#pragma unroll
-  for (int w = 0; w < W; ++w)
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (n0 + col + i >= p.N) v[w][i] = 0.f;
+  // columns past N took the last row's weights: finish8 clears or leaves them out
   finish8<T, E>(p, token, n0 + col, v[0], v[W - 1], Saved{});
 }
 

@@ -135,6 +135,15 @@ __device__ __forceinline__ Saved load_saved(const Product& p, int64_t m, int n) 
   return {load_raw((const T*)p.in + m * p.ld_io, n, p.N), load_raw((const T*)p.in2 + m * p.ld_io, n, p.N)};
 }
 
+// Zeros for what lies past the product's columns: there a row of infinities met the weights' padding, and its NaN
+// would reach the whole row through the next product.
+__device__ __forceinline__ void clear_padding(const Product& p, int n, float* v) {
+  if (n + 8 <= p.N) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (n + i >= p.N) v[i] = 0.f;
+}
+
 // Columns n .. n + 7 of row m of the product: v (Gate: the gate's v, the up's w).
 template <typename T, Epi E>
 __device__ __forceinline__ void finish8(const Product& p, int64_t m, int n, float* v, const float* w, const Saved& io) {
@@ -163,6 +172,7 @@ __device__ __forceinline__ void finish8(const Product& p, int64_t m, int n, floa
     activate<8, false>(v, p.act, v, nullptr);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= w[i];
+    clear_padding(p, n, v);
     store_chunk((T*)p.out + m * p.ld_out, n, p.pad_n, v);
   } else {
     float g[8], u[8], h[8], slope[8];
@@ -181,6 +191,9 @@ __device__ __forceinline__ void finish8(const Product& p, int64_t m, int n, floa
       h[i] = a * u[i];
       u[i] = v[i] * a;
     }
+    clear_padding(p, n, g);
+    clear_padding(p, n, u);
+    clear_padding(p, n, h);
     store_chunk((T*)p.out + m * p.ld_out, n, p.pad_n, g);
     store_chunk((T*)p.out2 + m * p.ld_out, n, p.pad_n, u);
     store_chunk((T*)p.out3 + m * p.ld_out, n, p.pad_n, h);

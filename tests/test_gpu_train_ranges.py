@@ -148,6 +148,29 @@ def test_ffn_offsets_past_32_bits(T):
         ref.assert_within("backward", got, w, b, got.dtype)
 
 
+# ------------------------------------------------------------------ infinities
+
+@pytest.mark.parametrize("T,D,F", [(1, 16, 3), (5, 16, 3), (16, 13, 11), (20, 16, 3), (40, 13, 11), (40, 16, 24), (300, 520, 1003)])
+def test_ffn_infinite_rows_of_positive_weights_stay_infinite(T, D, F):
+    """Where no infinities cancel, the definition gives infinity: nothing that pads a matrix makes NaN of it."""
+    g = _gen("infinite", T, D, F)
+    dt = torch.bfloat16
+    wg, wu, wd = ((0.5 + torch.rand(*s, generator=g, device=DEV)).to(dt) for s in ((F, D), (F, D), (D, F)))
+    x, dy = torch.zeros(T, D, dtype=dt, device=DEV), torch.zeros(T, D, dtype=dt, device=DEV)
+    x[:, 1], dy[:, 1] = 1 / F, 1 / F
+    x[T // 2, D - 1], dy[T // 2, 0] = math.inf, math.inf
+    gate, up = (torch.ones(T, F, dtype=dt, device=DEV) for _ in range(2))
+    rest = torch.arange(T, device=DEV) != T // 2
+    ws = train.gated_ffn_workspace(T, D, F, dt, backward=True)
+    for act in ("silu", "gelu"):
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        grads = [torch.empty_like(w) for w in (wg, wu, wd)]
+        train.gated_ffn(x, wg, wu, wd, y, ws, act=act)
+        assert bool((y[T // 2] == math.inf).all()) and bool(y[rest].isfinite().all())
+        train.gated_ffn_backward(dy, x.nan_to_num(posinf=1.0), gate, up, wg, wu, wd, dx, *grads, ws, act=act)
+        assert bool((dx[T // 2] == math.inf).all()) and bool(dx[rest].isfinite().all())
+
+
 # ------------------------------------------------------------------ activations
 
 def _activation(g, name):
